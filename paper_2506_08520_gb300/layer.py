@@ -26,6 +26,7 @@ from .binding import _DTYPE_CODE, NYSTRA_OK, NystraError, _stream_ptr, lib
 
 ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
 LINEAR_MAX_D, ROTARY_MAX_D = 128, 256
+_INT_MAX = 2 ** 31 - 1
 
 
 # What a call checks of its tensors' shapes, strides and dtypes, and derives from them alone, is kept by
@@ -82,6 +83,13 @@ def _shaped(name, t, shape, kind=None):
         raise ValueError(f"{name} must be contiguous, of {kind}")
     if kind is None and t[1][-1] != 1 and shape[-1] > 1 and 0 not in shape:
         raise ValueError(f"{name}: features (the last axis) must be adjacent")
+
+
+def _sizes_fit(**sizes):
+    """The C entries take these as 32-bit integers, and ctypes would cut a larger one off without a word."""
+    for name, size in sizes.items():
+        if size > _INT_MAX:
+            raise ValueError(f"{name} = {size}: at most {_INT_MAX}")
 
 
 def _on(x, stream, call):
@@ -160,6 +168,7 @@ def _norm_plan(x, weight, bias, out, dy):
     """(dtype codes of x and of the parameters, rows, C, row strides of x, out, dy, bytes of the backward workspace)."""
     dt = _dtype(x, out, dy)
     C = x[0][-1] if len(x[0]) else 0
+    _sizes_fit(C=C)
     kind = None
     for p in (weight, bias):
         if p is None:
@@ -290,6 +299,7 @@ def _rotary_plan(q, k, inv_freq, positions, out_q, out_k, layout):
     if len(inv_freq[0]) != 1:
         raise ValueError("inv_freq must have one axis")
     _shaped("inv_freq", inv_freq, tuple(inv_freq[0]), torch.float64)
+    _sizes_fit(n=n, heads=max(x[2] for x in rows), N=N, d=d, rotary_dim=2 * inv_freq[0][0])
     if layout not in ROTARY_LAYOUTS:
         raise ValueError(f"unknown layout {layout!r}")
     bits = step = 0
@@ -352,6 +362,7 @@ def _sizes(q, v, axes):
     dk, dv = q[0][-1], v[0][-1]
     if not (1 <= dk <= LINEAR_MAX_D and 1 <= dv <= LINEAR_MAX_D):
         raise ValueError(f"d_k and d_v must lie in 1..{LINEAR_MAX_D}")
+    _sizes_fit(**dict(zip(("n", "heads", "N"), q[0][:-1])))
     return tuple(q[0][:-1]), dk, dv
 
 

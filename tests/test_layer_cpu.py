@@ -115,3 +115,32 @@ def test_rotary_frequencies():
                 dict(rotary_dim=8, scaling="yarn", factor=2)):
         with pytest.raises(ValueError):
             pn.rotary_frequencies(**bad, device="cpu")
+
+
+@pytest.mark.parametrize("big", [2 ** 31, 2 ** 32 + 8])
+def test_sizes_beyond_32_bits_are_refused(big):
+    """The C entries take sizes of 32 bits: a larger one must not reach them, where only its low bits would count."""
+    ld, inv = sig(1, dtype=torch.float32), sig(1, dtype=torch.float64)
+    long, many, wide = sig(1, 1, big, 2), sig(big, 1, 1, 2), sig(1, big, 1, 2)
+    for x in (long, many, wide):
+        heads = sig(x[0][1], dtype=torch.float32)
+        with pytest.raises(ValueError, match="at most"):
+            layer._linear_plan(x, x, x, None, heads, None, None, None, None, 0)
+        with pytest.raises(ValueError, match="at most"):
+            layer._linear_plan(x, x, x, x, heads, None, None, None, None, 1)
+        for k in (None, x):
+            with pytest.raises(ValueError, match="at most"):
+                layer._rotary_plan(x, k, inv, None, None, None, "half")
+    with pytest.raises(ValueError, match="at most"):  # the keys' heads alone
+        layer._rotary_plan(sig(1, 1, 1, 2), wide, inv, None, None, None, "half")
+    with pytest.raises(ValueError, match="at most"):  # a table as long as the head of 2 that its low bits would fit
+        layer._rotary_plan(sig(1, 1, 1, 2), None, sig(big, dtype=torch.float64), None, None, None, "half")
+    for x in (sig(big, 1, 2), sig(1, big, 2)):
+        heads = sig(x[0][1], dtype=torch.float32)
+        state = sig(*x[0][:2], 2, 2, dtype=torch.float32)
+        with pytest.raises(ValueError, match="at most"):
+            layer._step_plan(x, x, x, heads, state, state, None)
+    for w in (None, sig(big)):
+        with pytest.raises(ValueError, match="at most"):
+            layer._norm_plan(sig(1, big), w, None, None, None)
+    assert layer._norm_plan(sig(big, 1), None, None, None, None)[2] == big  # rows are 64 bits there
