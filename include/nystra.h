@@ -376,8 +376,9 @@ NYSTRA_API long long nystra_debug_stages_size(int N, int d_h, int m);
  *  weight, bias  [C] of type w_dtype (fp32, or dtype), each may be null.
  *  mean, rstd    [rows] fp32, each may be null: mean and 1 / sqrt(var + eps),
  *            which the backward pass reads.
- *  rows >= 0, C >= 0, eps >= 0 and finite.
+ *  rows >= 0, C 0..NYSTRA_LAYER_NORM_MAX_C, eps >= 0 and finite.
  */
+#define NYSTRA_LAYER_NORM_MAX_C 1073741824
 NYSTRA_API int nystra_layer_norm(const void* x, long long x_stride, const void* weight, const void* bias, void* y,
                                  long long y_stride, float* mean, float* rstd, long long rows, int C, float eps,
                                  int dtype, int w_dtype, void* stream);
@@ -399,7 +400,7 @@ NYSTRA_API int nystra_layer_norm_backward(const void* dy, long long dy_stride, c
                                           long long dx_stride, void* dweight, void* dbias, long long rows, int C,
                                           int dtype, int w_dtype, void* workspace, long long workspace_bytes,
                                           void* stream);
-/* Bytes of workspace for (rows, C); NYSTRA_EINVAL (negative) for negative sizes.  Touches no device. */
+/* Bytes of workspace for (rows, C); NYSTRA_EINVAL (negative) for sizes that the calls refuse.  Touches no device. */
 NYSTRA_API long long nystra_layer_norm_workspace(long long rows, int C);
 
 /* Which features of a head form the pairs that turn together, i < rotary_dim / 2. */

@@ -20,6 +20,9 @@ using nystra::Strided;
 bool dtype_ok(int dtype) { return dtype == NYSTRA_F32 || dtype == NYSTRA_BF16 || dtype == NYSTRA_F16; }
 bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
+// Sizes of the norm's calls.  Columns, and a partial row's 2 C sums, are indexed with 32 bits.
+bool norm_sizes(long long rows, int C) { return rows >= 0 && C >= 0 && C <= NYSTRA_LAYER_NORM_MAX_C; }
+
 // Memory from a tensor's first to behind its last element.
 struct Span {
     const void* p;
@@ -140,7 +143,7 @@ int nystra_layer_norm(const void* x, long long x_stride, const void* weight, con
                       long long y_stride, float* mean, float* rstd, long long rows, int C, float eps, int dtype,
                       int w_dtype, void* stream) {
     if (!dtype_ok(dtype) || (w_dtype != NYSTRA_F32 && w_dtype != dtype)) return NYSTRA_EDTYPE;
-    if (rows < 0 || C < 0 || !(eps >= 0.f) || !isfinite(eps)) return NYSTRA_EINVAL;
+    if (!norm_sizes(rows, C) || !(eps >= 0.f) || !isfinite(eps)) return NYSTRA_EINVAL;
     if (rows == 0 || C == 0) return NYSTRA_OK;
     const size_t es = elem_size(dtype), ws = elem_size(w_dtype);
     const Tensor tx(x, &x_stride, {rows}, C, es), ty(y, &y_stride, {rows}, C, es);
@@ -157,7 +160,7 @@ int nystra_layer_norm(const void* x, long long x_stride, const void* weight, con
 }
 
 long long nystra_layer_norm_workspace(long long rows, int C) {
-    if (rows < 0 || C < 0) return NYSTRA_EINVAL;
+    if (!norm_sizes(rows, C)) return NYSTRA_EINVAL;
     return (long long)layer_norm_parts(rows, C) * 2 * C * 4;
 }
 
@@ -166,7 +169,7 @@ int nystra_layer_norm_backward(const void* dy, long long dy_stride, const void* 
                                void* dweight, void* dbias, long long rows, int C, int dtype, int w_dtype,
                                void* workspace, long long workspace_bytes, void* stream) {
     if (!dtype_ok(dtype) || (w_dtype != NYSTRA_F32 && w_dtype != dtype)) return NYSTRA_EDTYPE;
-    if (rows < 0 || C < 0) return NYSTRA_EINVAL;
+    if (!norm_sizes(rows, C)) return NYSTRA_EINVAL;
     if (C == 0) return NYSTRA_OK;
     const size_t es = elem_size(dtype), ws = elem_size(w_dtype);
     if (!aligned(weight, ws) || !aligned(dweight, ws) || !aligned(dbias, ws)) return NYSTRA_EINVAL;

@@ -184,7 +184,10 @@ def _norm_plan(x, weight, bias, out, dy):
         if t is not None and t[0] != x[0]:
             raise ValueError(f"{name} must have x's shape")
         strides.append(C if t is None else _rows(t[0], t[1])[1])
-    return dt, _DTYPE_CODE[x[2] if kind is None else kind], rows, C, xs, *strides, lib().nystra_layer_norm_workspace(rows, C)
+    need = lib().nystra_layer_norm_workspace(rows, C)
+    if need < 0:
+        raise NystraError(int(need), "nystra_layer_norm_workspace")
+    return dt, _DTYPE_CODE[x[2] if kind is None else kind], rows, C, xs, *strides, need
 
 
 def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,

@@ -160,3 +160,16 @@ def step(L, q=A, qs=(64, 32), k=B, ks=(64, 32), v=C, vs=(64, 32), o=D, os=(64, 3
     (dict(n=0, q=0), OK)])
 def test_linear_attention_step(lib, kw, code):
     assert step(lib, **kw) == code
+
+
+@pytest.mark.parametrize("cols", [(1 << 30) + 1, (1 << 31) - 600, (1 << 31) - 1])
+def test_layer_norm_rows_too_long(lib, cols):
+    """Rows whose columns, or the two sums per column, would leave 32-bit indexes."""
+    far = dict(xs=1 << 31, ys=1 << 31)
+    wide = {k: i << 40 for i, k in enumerate("xwbymr", 1)}
+    assert norm(lib, cols=cols, **far, **wide) == EINVAL
+    assert lib.nystra_layer_norm_workspace(4, cols) == EINVAL
+    wide = {k: i << 40 for i, k in enumerate(("dy", "x", "m", "r", "w", "dx", "dw", "db", "ws"), 1)}
+    for grads in ({}, dict(dw=0, db=0, ws=0)):
+        assert norm_bwd(lib, cols=cols, ds=1 << 31, xs=1 << 31, dxs=1 << 31, wb=1 << 40, **{**wide, **grads}) == EINVAL
+    assert lib.nystra_layer_norm_workspace(4, 1 << 30) > 0

@@ -144,3 +144,8 @@ def test_sizes_beyond_32_bits_are_refused(big):
         with pytest.raises(ValueError, match="at most"):
             layer._norm_plan(sig(1, big), w, None, None, None)
     assert layer._norm_plan(sig(big, 1), None, None, None, None)[2] == big  # rows are 64 bits there
+
+
+def test_norm_rows_too_long():
+    with pytest.raises(pn.NystraError):
+        layer._norm_plan(sig(1, 2 ** 30 + 1), None, None, None, None)
