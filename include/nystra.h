@@ -418,7 +418,10 @@ typedef enum {
  *  q, q_out  [n, q_heads, N, d] with three strides each; k, k_out the same
  *            with k_heads (0: no keys, the pointers are not looked at).
  *            q_out may be q itself, and k_out k (same strides); then q and k
- *            may be slices of one buffer, but may not share elements.
+ *            may be slices of one buffer, but may not share elements: layouts
+ *            that may are refused (known not to: one behind the other, or
+ *            slices like a fused projection's, sequence by sequence or token
+ *            by token or head by head).
  *  inv_freq  [rotary_dim / 2] fp64, finite: radians per position.  Angles are
  *            accurate to about 2^-53 |p inv_freq| + 2^-24 radians.
  *  positions [N], or [n, N] with positions_stride elements between sequences

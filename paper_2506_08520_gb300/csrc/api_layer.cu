@@ -81,6 +81,43 @@ struct Tensor {
     Strided strided() const { return {stride[0], stride[1], stride[2]}; }
 };
 
+// Whether two tensors [n, heads, N, d] of one type are known to share no element.  By the axes in the order
+// of their strides: what the inner ones reach is an interval of its own in either tensor, and each outer
+// axis, which steps alike in both, steps over the two intervals and all that the axes inside it reach.  With
+// every axis inside, that is two tensors one behind the other; with the heads inside, slices of a fused
+// projection.
+bool disjoint(const Tensor& a, const Tensor& b) {
+    const __int128 off = ((__int128)(intptr_t)b.p - (intptr_t)a.p) / (long long)a.es;
+    long long step[2][3];
+    for (int i = 0; i < 3; ++i) {  // an axis of one element steps like the other tensor's
+        step[0][i] = a.size[i] > 1 ? a.stride[i] : b.size[i] > 1 ? b.stride[i] : 0;
+        step[1][i] = b.size[i] > 1 ? b.stride[i] : step[0][i];
+    }
+    int order[3] = {0, 1, 2};
+    std::sort(order, order + 3, [&](int x, int y) {
+        return std::max(step[0][x], step[1][x]) < std::max(step[0][y], step[1][y]);
+    });
+    for (int inner = 0; inner <= 3; ++inner) {
+        __int128 ra = a.d, rb = b.d;
+        for (int i = 0; i < inner; ++i) {
+            const int x = order[i];
+            ra += (__int128)(a.size[x] - 1) * step[0][x];
+            rb += (__int128)(b.size[x] - 1) * step[1][x];
+        }
+        bool ok = off >= ra || -off >= rb;
+        __int128 reach = off >= 0 ? std::max(ra, off + rb) : std::max(rb, ra - off);
+        for (int i = inner; i < 3; ++i) {
+            const int x = order[i];
+            const long long most = std::max(a.size[x], b.size[x]);
+            if (most < 2) continue;
+            ok = ok && step[0][x] == step[1][x] && step[0][x] >= reach;
+            reach += (__int128)(most - 1) * step[0][x];
+        }
+        if (ok) return true;
+    }
+    return false;
+}
+
 Span flat(const void* p, size_t bytes) { return {p, p ? bytes : 0}; }
 
 bool any_meet(const Span& out, std::initializer_list<Span> others) {
@@ -235,8 +272,8 @@ int nystra_rotary(const void* q, const long long* q_strides, void* q_out, const 
         if ((!in_place[i] && s.meets(x[i].span())) || any_meet(s, {table, pos})) return NYSTRA_EINVAL;
     }
     if (q_heads && k_heads) {  // in place, q and k may be interleaved slices of one buffer
-        const bool both = in_place[0] && in_place[1];
-        if (both ? x[0].p == x[1].p : y[0].span().meets(y[1].span())) return NYSTRA_EINVAL;
+        if ((in_place[0] || in_place[1]) && !disjoint(x[0], x[1])) return NYSTRA_EINVAL;
+        if (!(in_place[0] && in_place[1]) && y[0].span().meets(y[1].span())) return NYSTRA_EINVAL;
         if (!in_place[0] && y[0].span().meets(x[1].span())) return NYSTRA_EINVAL;
         if (!in_place[1] && y[1].span().meets(x[0].span())) return NYSTRA_EINVAL;
     }

@@ -352,7 +352,8 @@ def rotary(x: torch.Tensor, inv_freq: torch.Tensor, positions: torch.Tensor | No
 def rotary_qk(q: torch.Tensor, k: torch.Tensor, inv_freq: torch.Tensor, positions: torch.Tensor | None = None,
               layout: str = "half", amplitude: float = 1.0, inverse: bool = False, out=None, stream=None):
     """``rotary`` of queries and keys in one launch: ``(q', k')``.  Their numbers of
-    heads may differ.  ``out`` may give the two results; ``(q, k)`` turns them in place."""
+    heads may differ.  ``out`` may give the two results; ``(q, k)`` turns them in place,
+    where they may be slices of one buffer but share no elements."""
     return tuple(_rotary(q, k, inv_freq, positions, layout, amplitude, inverse, (None, None) if out is None else out,
                          stream))
 

@@ -173,3 +173,27 @@ def test_layer_norm_rows_too_long(lib, cols):
     for grads in ({}, dict(dw=0, db=0, ws=0)):
         assert norm_bwd(lib, cols=cols, ds=1 << 31, xs=1 << 31, dxs=1 << 31, wb=1 << 40, **{**wide, **grads}) == EINVAL
     assert lib.nystra_layer_norm_workspace(4, 1 << 30) > 0
+
+
+# q and k [2, heads, 5, d = 64] in one buffer, k `at` elements behind q, which share elements
+@pytest.mark.parametrize("qs,ks,at,hq,hk", [
+    ((3840, 64, 768), (3840, 64, 768), 64, 4, 4),     # a fused projection [n, N, 3, heads, d], k one head on
+    ((3840, 64, 768), (3840, 64, 768), 192, 4, 2),    # three heads on
+    ((3840, 64, 768), (3840, 64, 768), 768, 4, 4),    # one token on
+    ((3840, 64, 768), (3840, 64, 768), 3840, 4, 4),   # one sequence on
+    ((3840, 64, 768), (3840, 64, 768), 2, 4, 4),      # one pair of features on
+    ((3840, 64, 768), (3840, 64, 768), 254, 4, 4),    # one pair of features short of the next place
+    ((3840, 64, 768), (3840, 64, 768), 0, 4, 4),
+    ((3840, 64, 768), (3840, 64, 768), 0, 4, 1),
+    ((2560, 64, 512), (2560, 64, 512), 384, 4, 4),    # q's heads of the next token
+    ((1280, 64, 256), (1280, 256, 64), 256, 4, 4),    # other strides
+])
+def test_rotary_in_place_on_shared_elements(lib, qs, ks, at, hq, hk):
+    """Turned in place, q and k may be slices of one buffer, but each element turns once: refused, whichever comes
+    first, and also where only one of them is turned in place and the other one reads."""
+    k = A + 2 * at
+    a = dict(q=A, qo=A, qs=qs, qos=qs, hq=hq, k=k, ko=k, ks=ks, kos=ks, hk=hk)
+    b = dict(q=k, qo=k, qs=ks, qos=ks, hq=hk, k=A, ko=A, ks=qs, kos=qs, hk=hq)
+    for args in (a, b):
+        for other in ({}, dict(qo=C), dict(ko=C)):
+            assert rot(lib, n=2, N=5, pos=None, f=K, **{**args, **other}) == EINVAL
