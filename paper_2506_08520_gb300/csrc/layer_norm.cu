@@ -13,10 +13,10 @@
 // Both directions are bound by memory: 2 (forward) and 3 (backward) elements
 // moved per element, about 8 and 14 operations.  Measured: forward of 262144 rows of
 // 180 in bf16 35 us (5.4 TB/s; loads without copies ahead 46 at 64 registers, 38 at 88),
-// backward of 16384 x 4096 in bf16 91 us + 6 for the sums (4.4 TB/s).  The backward
-// pass issues 390 instructions a thread and row at 15 warps an SM (118 registers): 47% of
-// the issue slots, waiting for its shuffles and shared memory; weights in shared memory
-// instead of registers give three CTAs an SM and are slower all the same (115 us).
+// backward of 16384 x 4096 in bf16 94 us a call, 6 of them for the sums (4.3 TB/s).  The backward
+// pass waits for its shuffles and shared memory at 15 warps an SM (two CTAs by registers); xh, formed once
+// a row, takes the registers of x (formed again for dx: 100 us).  Weights in shared memory
+// instead of registers give three CTAs an SM and were slower all the same.
 #include "common.cuh"
 #include "layer.cuh"
 #include "pack.cuh"
@@ -391,19 +391,21 @@ __global__ void __launch_bounds__(cta_threads(TPR)) layer_norm_backward_kernel(c
             }
         }
         d = d == kAhead - 1 ? 0 : d + 1;
-        // xh = x rstd - mean rstd
-        const uint64_t scale = pack_x2(rstd, rstd), shift = pack_x2(-mean * rstd, -mean * rstd);
-        uint64_t s0 = 0ull, s1 = 0ull;
+        // xh = (x - mean) rstd: x rstd - mean rstd would be off by a rounding of the mean's size.  The
+        // second of a lone column stays 0, however large the mean.
+        const uint64_t scale = pack_x2(rstd, rstd), shift = pack_x2(-mean, VEC > 1 ? -mean : 0.f);
+        uint64_t s0 = 0ull, s1 = 0ull, xh[NV][H];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             // columns behind C must not meet a mean or rstd that is not finite
             if ((t + i * TPR) * VEC < a.C) {
 #pragma unroll
                 for (int e = 0; e < H; ++e) {
-                    const uint64_t f = pair(dy[i], e), xh = fma_x2(pair(x[i], e), scale, shift), g = mul_x2(f, w[i][e]);
+                    const uint64_t f = pair(dy[i], e), g = mul_x2(f, w[i][e]);
+                    xh[i][e] = mul_x2(add_x2(pair(x[i], e), shift), scale);
                     s0 = add_x2(s0, g);
-                    s1 = fma_x2(g, xh, s1);
-                    dw[i][e] = fma_x2(f, xh, dw[i][e]);
+                    s1 = fma_x2(g, xh[i][e], s1);
+                    dw[i][e] = fma_x2(f, xh[i][e], dw[i][e]);
                     db[i][e] = add_x2(db[i][e], f);
                 }
             }
@@ -421,8 +423,8 @@ __global__ void __launch_bounds__(cta_threads(TPR)) layer_norm_backward_kernel(c
             P o;
 #pragma unroll
             for (int e = 0; e < H; ++e) {
-                const uint64_t xh = fma_x2(pair(x[i], e), scale, shift), g = mul_x2(pair(dy[i], e), w[i][e]);
-                const float2 y = unpack_x2(fma_x2(g, scale, fma_x2(xh, k2, k1)));
+                const uint64_t g = mul_x2(pair(dy[i], e), w[i][e]);
+                const float2 y = unpack_x2(fma_x2(g, scale, fma_x2(xh[i][e], k2, k1)));
                 o.v[2 * e] = from_f32<T>(y.x);
                 if (2 * e + 1 < VEC) o.v[2 * e + 1 < VEC ? 2 * e + 1 : 0] = from_f32<T>(y.y);
             }
