@@ -375,7 +375,8 @@ NYSTRA_API long long nystra_debug_stages_size(int N, int d_h, int m);
  *            y_stride >= C unless rows = 1.  y may be x itself (same strides).
  *  weight, bias  [C] of type w_dtype (fp32, or dtype), each may be null.
  *  mean, rstd    [rows] fp32, each may be null: mean and 1 / sqrt(var + eps),
- *            which the backward pass reads.
+ *            which the backward pass reads.  C = 0: a no-op, these two stay as
+ *            they are.
  *  rows >= 0, C 0..NYSTRA_LAYER_NORM_MAX_C, eps >= 0 and finite.
  */
 #define NYSTRA_LAYER_NORM_MAX_C 1073741824

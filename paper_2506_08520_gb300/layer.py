@@ -194,8 +194,8 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.
                eps: float = 1e-5, out: torch.Tensor | None = None, return_stats: bool = False, stream=None):
     """Layer norm over the last axis of ``x`` ``[..., C]`` with optional ``weight``
     and ``bias`` ``[C]`` (fp32, or x's dtype).  ``out`` may be ``x`` itself.  With
-    ``return_stats``: ``(y, mean, rstd)``, the two fp32 per row, which
-    ``layer_norm_backward`` reads."""
+    ``return_stats``: ``(y, mean, rstd)``, the two fp32 per row (NaN where C is 0),
+    which ``layer_norm_backward`` reads."""
     _tensors(x, weight, bias, out)
     dt, wdt, rows, C, xs, ys, _, _ = _norm_plan(_sig(x), _sig(weight), _sig(bias), _sig(out), None)
 
@@ -205,6 +205,9 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.
         if return_stats:
             mean = _empty(x.shape[:-1], x, torch.float32)
             rstd = torch.empty_like(mean)
+            if not C:  # the C entry writes nothing where rows have no values, whose mean is no number
+                mean.fill_(math.nan)
+                rstd.fill_(math.nan)
         _raise(lib().nystra_layer_norm(x.data_ptr(), xs, _ptr(weight), _ptr(bias), y.data_ptr(), ys, _ptr(mean),
                                        _ptr(rstd), rows, C, eps, dt, wdt, st), "nystra_layer_norm")
         return (y, mean, rstd) if return_stats else y
