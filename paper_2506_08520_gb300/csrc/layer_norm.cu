@@ -563,17 +563,35 @@ int pack_of(int C, long long strides, uintptr_t pointers) {
 struct RowShape {
     int threads, nv;
 };
-RowShape row_shape(int packs, int most) {
+constexpr RowShape row_shape(int packs, int most) {
     for (int threads : {8, 16, 32, 128, 256, 512})
         for (int nv = 1; nv <= most; ++nv)
             if (packs <= threads * nv && (nv < 4 || threads >= 32)) return {threads, nv};
     return {0, 0};
 }
-#define NYSTRA_ROWS(ROW)                                                        \
-    ROW(8, 1) ROW(8, 2) ROW(8, 3) ROW(16, 1) ROW(16, 2) ROW(16, 3)              \
-    ROW(32, 1) ROW(32, 2) ROW(32, 3) ROW(32, 4) ROW(128, 1) ROW(128, 2)         \
-    ROW(128, 3) ROW(128, 4) ROW(256, 1) ROW(256, 2) ROW(256, 3) ROW(256, 4)     \
-    ROW(512, 1) ROW(512, 2) ROW(512, 3) ROW(512, 4)
+// Whether a row takes this shape: if any does, the longest that it covers.
+constexpr bool row_taken(int threads, int nv, int most) {
+    const RowShape s = row_shape(threads * nv, most);
+    return s.threads == threads && s.nv == nv;
+}
+// The shapes that rows take with two packs at most or with four: no kernel is built that no call reaches.
+#define NYSTRA_ROWS(ROW)                                                       \
+    ROW(8, 1) ROW(8, 2) ROW(8, 3) ROW(16, 2) ROW(16, 3) ROW(32, 2) ROW(32, 3)  \
+    ROW(32, 4) ROW(128, 1) ROW(128, 2) ROW(128, 3) ROW(128, 4) ROW(256, 2)     \
+    ROW(256, 3) ROW(256, 4) ROW(512, 2) ROW(512, 3) ROW(512, 4)
+#define NYSTRA_ROW(TPR, NV) static_assert(row_taken(TPR, NV, 2) || row_taken(TPR, NV, 4), "no row takes this shape");
+NYSTRA_ROWS(NYSTRA_ROW)
+#undef NYSTRA_ROW
+// ... and no row goes without: every shape that is taken has a kernel.
+#define NYSTRA_ROW(TPR, NV) +(row_taken(TPR, NV, MOST) ? 1 : 0)
+template <int MOST> constexpr bool rows_complete() {
+    int taken = 0;
+    for (int threads : {8, 16, 32, 128, 256, 512})
+        for (int nv = 1; nv <= MOST; ++nv) taken += row_taken(threads, nv, MOST);
+    return taken == 0 NYSTRA_ROWS(NYSTRA_ROW);
+}
+#undef NYSTRA_ROW
+static_assert(rows_complete<2>() && rows_complete<4>(), "a row's shape has no kernel");
 
 template <typename T, int VEC, int NV, int TPR>
 cudaError_t run_fwd(const NormFwd& a, int sms, cudaStream_t st) {
@@ -592,8 +610,9 @@ cudaError_t run_fwd(const NormFwd& a, int sms, cudaStream_t st) {
 template <typename T, int VEC>
 cudaError_t pick_fwd(const NormFwd& a, int sms, cudaStream_t st) {
     const RowShape s = row_shape(a.C / VEC, 4);
-#define NYSTRA_ROW(TPR, NV) \
-    if (s.threads == TPR && s.nv == NV) return run_fwd<T, VEC, NV, TPR>(a, sms, st);
+#define NYSTRA_ROW(TPR, NV)                    \
+    if constexpr (row_taken(TPR, NV, 4))       \
+        if (s.threads == TPR && s.nv == NV) return run_fwd<T, VEC, NV, TPR>(a, sms, st);
     NYSTRA_ROWS(NYSTRA_ROW)
 #undef NYSTRA_ROW
     const long long most = (long long)sms * 4;
@@ -637,8 +656,8 @@ cudaError_t pick_bwd(const NormBwd& a, int* grid, cudaStream_t st) {
     // Sums, weights and values of 16 columns at most: more leave too few registers for two CTAs on an SM.
     constexpr int MOST = VEC == 8 ? 2 : 4;
     const RowShape s = row_shape(a.C / VEC, MOST);
-#define NYSTRA_ROW(TPR, NV)                                  \
-    if constexpr (NV <= MOST)                                \
+#define NYSTRA_ROW(TPR, NV)                    \
+    if constexpr (row_taken(TPR, NV, MOST))    \
         if (s.threads == TPR && s.nv == NV) return run_bwd<T, VEC, NV, TPR>(a, grid, st);
     NYSTRA_ROWS(NYSTRA_ROW)
 #undef NYSTRA_ROW
