@@ -460,6 +460,11 @@ NYSTRA_API int nystra_rotary(const void* q, const long long* q_strides, void* q_
  * 16-bit types enter the tensor cores as they are; on the way to a 16-bit result
  * the masked scores, and the state where it meets the queries, are rounded to
  * that type, each by half a step (the state that is carried and returned is not).
+ * Not so in the first 64 tokens of a sequence without state_in (for the gradients
+ * of k and v: in the last 64 of one without dstate_out), whose results are sums of
+ * few terms: there the scores carry two parts, and a result is off by its own
+ * rounding only.  A call with a state for a single token rounds the state;
+ * nystra_linear_attention_step does not.
  * fp32 operands are taken apart into 16-bit parts that carry all of them.
  * Values: finite.  One that is not makes the results of its 64 tokens and of all
  * later ones of its sequence and head undefined (nothing else); behind `lengths`

@@ -11,9 +11,10 @@
 // S^T a^T: the state never leaves the registers.  So the output is formed as
 // out^T = S^T a^T + c^T P^T, with P made by all warps together in shared memory.
 //
-// 16-bit types.  Roundings to 16 bits, each by half a step: P (two parts of it in a
-// sequence of one chunk, whose results may have a single term); S as an operand
-// (never the S that is carried); the result.  w_s c_s, the A operand of the state's
+// 16-bit types.  Roundings to 16 bits, each by half a step: P (but two parts of it in
+// the first chunk that a sequence visits, if no state enters it or it is the only one:
+// results of few terms would show the rounding as it is, not averaged over many); S as
+// an operand (never the S that is carried); the result.  w_s c_s, the A operand of the state's
 // product, is split into 16-bit parts: two where the state is only read again as
 // such an operand, and in bf16 three, which carry all of fp32, where it is returned.
 // fp16: P, S and w c are scaled by powers of two that put the largest of them
@@ -325,7 +326,9 @@ struct ChunkShape {
     static constexpr int kTile = kChunk * DP;  // values of one part of a tile
     static constexpr int kTiles = Io::kStages * 3 * Io::kParts * kTile;
     static constexpr int kScores = Io::kParts * kBlocks * kBlock;
-    static constexpr size_t kSmem = (kTiles + kScores) * 2 + sizeof(ChunkTables);
+    // In front of the tiles: room for what the first chunk's low part of P has more than its tile of a
+    static constexpr int kPad = Io::kParts == 1 && kTile < kScores ? kScores - kTile : 0;
+    static constexpr size_t kSmem = (kPad + kTiles + kScores) * 2 + sizeof(ChunkTables);
     // CTAs per SM that registers are cut for: 16 warps of 128, or what the fp32 tiles leave room for
     static constexpr int kResident = Io::kParts == 1 ? 16 / kWarps : 128 / DP;
 };
@@ -414,7 +417,7 @@ linear_chunk_kernel(const __grid_constant__ LinArgs args) {
     constexpr bool SCALED = Op::kNarrowRange, SMALL = Io::kParts > 1;
     constexpr int THREADS = Shape::kThreads, NW = Shape::kWarps, IN = Io::kParts, TILE = Shape::kTile;
     extern __shared__ __align__(1024) unsigned char smem[];
-    E* const tiles = reinterpret_cast<E*>(smem);  // stages of a, b, c
+    E* const tiles = reinterpret_cast<E*>(smem) + Shape::kPad;  // stages of a, b, c
     E* const tp = tiles + Shape::kTiles;
     ChunkTables& tab = *reinterpret_cast<ChunkTables*>(tp + Shape::kScores);
 
@@ -450,10 +453,9 @@ linear_chunk_kernel(const __grid_constant__ LinArgs args) {
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
     const int chunks = live > u0 ? (live - u0 + kChunk - 1) / kChunk : 0;
-    // A single chunk leaves the other stage free for a second part of P: a result of few terms would
-    // show P's rounding as it is, not averaged over them.
-    const bool fine = Io::kStages == 2 && chunks == 1;
-    E* const tp_low = tiles + 3 * IN * TILE;
+    // The second part that P has in the first chunk: in the stage that a single chunk leaves free, or
+    // in the place of a, which nobody reads any more once the scores are made and no state meets it.
+    E* const tp_low = chunks == 1 ? tiles + 3 * IN * TILE : tiles - Shape::kPad;
     if (Io::kStages == 2 && chunks > 0) load(0);
     for (int i = threadIdx.x; i < 2 * kChunk; i += THREADS) {
         const float p = decay.power(max(i - 16, 0));
@@ -467,8 +469,8 @@ linear_chunk_kernel(const __grid_constant__ LinArgs args) {
     const float* s_in = nullptr;
     bool t_in = false;
     if (MAIN) {
-        s_in = args.segs > 1 ? lin_ws(args, blockIdx.y, unit, seg)
-                             : r.s_in ? r.s_in + (long long)unit * r.db * r.dc : nullptr;
+        s_in = seg > 0 || (args.segs > 1 && r.s_in) ? lin_ws(args, blockIdx.y, unit, seg)
+               : r.s_in ? r.s_in + (long long)unit * r.db * r.dc : nullptr;
         t_in = args.segs == 1 && r.transposed;
     }
 #pragma unroll
@@ -484,6 +486,8 @@ linear_chunk_kernel(const __grid_constant__ LinArgs args) {
 
     for (int i = 0; i < chunks; ++i) {
         const int cnt = min(live - u0 - i * kChunk, kChunk);
+        // whether P has two parts: in the first chunk that the sequence visits
+        [[maybe_unused]] const bool fine = IN == 1 && u0 == 0 && i == 0 && (chunks == 1 || !has_state);
         E *ta = stage(i), *tb = ta + IN * TILE, *tc = ta + 2 * IN * TILE;
         if constexpr (Io::kStages == 1) {
             __syncthreads();  // the last chunk's readers are done
@@ -536,6 +540,8 @@ linear_chunk_kernel(const __grid_constant__ LinArgs args) {
                 if (lane == 0) atomicMax(tab.top, __float_as_uint(most));
                 __syncthreads();
                 ep = to_2_14(__uint_as_float(tab.top[0]));
+            } else if (fine && chunks > 1) {
+                __syncthreads();  // a has been read
             }
             const float up = SCALED ? pow2i(ep) : 1.f;
 #pragma unroll
@@ -635,7 +641,8 @@ linear_chunk_kernel(const __grid_constant__ LinArgs args) {
                 }
             }
             if constexpr (SMALL) join(o, os);
-            const float down = SCALED ? pow2i(-ep) : 1.f;
+            if (fine && chunks > 1) __syncthreads();  // P's second part has been read
+            [[maybe_unused]] const float down = SCALED ? pow2i(-ep) : 1.f;
             T* const to = reinterpret_cast<T*>(ta);
             if constexpr (sizeof(T) == 2) {
 #pragma unroll

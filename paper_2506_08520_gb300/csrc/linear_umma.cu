@@ -51,8 +51,11 @@ constexpr int DP = 128;
 constexpr int kCollect = 256, kScore = 256, kSplit = 256, kThreads = kCollect + kScore + kSplit + 128;
 constexpr int kPanelB = kChunk * 128, kTileB = 2 * kPanelB, kStages = 3;
 constexpr int oOut = kStages * 3 * kTileB, oP = oOut + 2 * kTileB, oPower = oP + 2 * kPanelB,
-              oBar = oPower + (kChunk + 4 + 80) * 4, kSmem = oBar + 256 + 1024;  // 1024: room to align the start
+              oBar = oPower + (kChunk + 4 + 80) * 4, oLow = (oBar + 256 + 1023) / 1024 * 1024;
 static_assert(oBar % 16 == 0, "");
+// Without and with room for a second part of P; 1024: room to align the start
+constexpr int kSmem = oBar + 256 + 1024, kSmemFine = oLow + kPanelB + 1024;
+constexpr uint32_t kLow = oLow - oP;  // from the first chunk's P to its second part
 // TMEM columns
 constexpr uint32_t cX = 0, cO = 64, cD = 128, cS = 256, cW = 320, kWCols = 96, kTmemCols = 512;
 constexpr uint64_t kWaitNs = 2000000000ull;
@@ -113,9 +116,10 @@ __device__ __forceinline__ void split_blocks(uint32_t tmem_w, const T* v, const 
 
 // Block `blk` of P, one of the ten on and under the diagonal or, backward in time, on and
 // above it.  lags[15 + x]: s_scale o_scale gamma^x, 0 for x < 0.  Columns from cnt on
-// are rows of b that are no tokens of the chunk.  LOW: P's second part goes to `low`.
+// are rows of b that are no tokens of the chunk.  LOW: P's second part goes kLow
+// bytes on.
 template <bool LOW>
-__device__ __forceinline__ void make_scores(T* tp, T* low, const T* ta, const T* tb, const float* lags, int blk,
+__device__ __forceinline__ void make_scores(T* tp, const T* ta, const T* tb, const float* lags, int blk,
                                             bool backward, int cnt, int lane) {
     const int g = lane >> 2, c2 = (lane & 3) * 2;
     const int lo = blk < 1 ? 0 : blk < 3 ? 1 : blk < 6 ? 2 : 3, sh = blk - lo * (lo + 1) / 2;
@@ -154,7 +158,7 @@ __device__ __forceinline__ void make_scores(T* tp, T* low, const T* ta, const T*
             uint32_t* const at =
                 reinterpret_cast<uint32_t*>((reinterpret_cast<uintptr_t>(to) ^ (nt * 16)) + e * 4 * 128);
             *at = part[0];
-            if constexpr (LOW) at[(low - tp) / 2] = part[1];
+            if constexpr (LOW) at[kLow / 4] = part[1];
         }
 }
 
@@ -167,9 +171,13 @@ __device__ __forceinline__ void arrive_warp(uint64_t* bar, int lane) {
 
 // MAIN: outputs, from the state that enters the segment.  Otherwise the
 // segment's own contribution to the state, from zero, into the workspace.
-// ONE: sequences of one chunk at most, P in two parts (linear_chunk.cuh), the second
-// in the buffer that no second chunk is there to use.
-template <bool MAIN, bool ONE>
+// FINE: P in two parts in the first chunk that a sequence visits (linear_chunk.cuh), if no
+// state enters it or it is the only one.  That code costs the other chunks nothing as a
+// template argument with a chunk of its own (223.8 us for the backward pass of 4 x 16 heads x
+// 4096 tokens of 128, with or without it; as a branch in the loop 243), but 8 KB more of
+// shared memory, and so less L1, cost a call that has no use for them 3% (2048 tokens with
+// states 136 -> 140 us): they are asked for where they are used.
+template <bool MAIN, bool FINE>
 __global__ void __launch_bounds__(kThreads, 1)
 linear_umma_kernel(const __grid_constant__ LinArgs args, const __grid_constant__ Maps maps, unsigned int* fault) {
     extern __shared__ unsigned char smem_raw[];
@@ -195,14 +203,15 @@ linear_umma_kernel(const __grid_constant__ LinArgs args, const __grid_constant__
     const float* s_in = nullptr;
     bool t_in = false;
     if (MAIN) {
-        s_in = args.segs > 1 ? lin_ws(args, blockIdx.y, unit, seg)
-                             : r.s_in ? r.s_in + (long long)unit * r.db * r.dc : nullptr;
+        s_in = seg > 0 || (args.segs > 1 && r.s_in) ? lin_ws(args, blockIdx.y, unit, seg)
+               : r.s_in ? r.s_in + (long long)unit * r.db * r.dc : nullptr;
         t_in = args.segs == 1 && r.transposed;
     }
     // Chunk i: its tokens, the first of them in memory, and whether its sum is wanted.
     const auto count = [&](int i) { return min(live - u0 - i * kChunk, kChunk); };
     const auto low = [&](int i) { return r.backward ? len - (u0 + i * kChunk + count(i)) : u0 + i * kChunk; };
     const auto summed = [&](int i) { return i + 1 < chunks || keep; };
+    const auto fine = [&](int i) { return FINE && i == 0 && u0 == 0 && (chunks == 1 || !s_in); };
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
@@ -227,6 +236,9 @@ linear_umma_kernel(const __grid_constant__ LinArgs args, const __grid_constant__
     // P's other triangle stays zero
     for (int i = threadIdx.x; i < 2 * kPanelB / 16; i += kThreads)
         reinterpret_cast<uint4*>(smem + oP)[i] = make_uint4(0u, 0u, 0u, 0u);
+    if constexpr (FINE)
+        for (int i = threadIdx.x; i < kPanelB / 16; i += kThreads)
+            reinterpret_cast<uint4*>(smem + oLow)[i] = make_uint4(0u, 0u, 0u, 0u);
     fence_proxy_async_smem();
     constexpr int kIssue = kCollect + kScore + kSplit;  // the thread that issues
     if (warp == kIssue / 32) {
@@ -281,13 +293,11 @@ linear_umma_kernel(const __grid_constant__ LinArgs args, const __grid_constant__
                             t5::mma_f16_ta(tmem + cX, tmem + cS + ks * 8,
                                            t5::sdesc_sw128(qa + (ks >> 2) * kPanelB + (ks & 3) * 32, 16, 1024), id_x,
                                            ks > 0);
-                    for (int ks = 0; ks < kChunk / 16; ++ks)
-                        t5::mma_f16(tmem + cO, t5::sdesc_sw128(va + ks * 2048, kPanelB, 1024),
-                                    t5::sdesc_sw128(pa + ks * 32, 16, 1024), id_o, ks > 0);
-                    if constexpr (ONE)
+                    for (int part = fine(i) ? 1 : 0; part >= 0; --part)
                         for (int ks = 0; ks < kChunk / 16; ++ks)
                             t5::mma_f16(tmem + cO, t5::sdesc_sw128(va + ks * 2048, kPanelB, 1024),
-                                        t5::sdesc_sw128(smem_addr(scores(i + 1)) + ks * 32, 16, 1024), id_o, true);
+                                        t5::sdesc_sw128(pa + part * kLow + ks * 32, 16, 1024), id_o,
+                                        ks > 0 || (part == 0 && fine(i)));
                     t5::commit(bar.outs + (i & 1));
                 }
                 t5::commit(bar.free + st);
@@ -381,20 +391,27 @@ linear_umma_kernel(const __grid_constant__ LinArgs args, const __grid_constant__
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsScore));
         if constexpr (MAIN) {
             const int first = warp - kCollect / 32;
-            for (int i = 0; i < chunks; ++i) {
+            // Chunk i's P; false where a wait gave up.  `two`: whether it has two parts.
+            const auto chunk = [&](int i, auto two) {
                 const int st = i % kStages;
                 // the tiles are there, and the products of chunk i - 2 have read the P that lies where this one will
                 if (!mbar_wait_bounded(bar.full + st, (i / kStages) & 1, kWaitNs) ||
                     (i >= 2 && !mbar_wait_bounded(bar.outs + (i & 1), ((i - 2) >> 1) & 1, kWaitNs)))
                     failed = true;
                 failed = __any_sync(0xffffffffu, failed);
-                if (failed) break;
+                if (failed) return false;
                 for (int blk = first; blk < kBlocks; blk += kScore / 32)
-                    make_scores<ONE>(scores(i), scores(i + 1), tile(st, 0), tile(st, 1), lags, blk, r.backward, count(i),
-                                     lane);
+                    make_scores<decltype(two)::value>(scores(i), tile(st, 0), tile(st, 1), lags, blk, r.backward,
+                                                      count(i), lane);
                 fence_proxy_async_smem();
                 arrive_warp(bar.scores + (i & 1), lane);
-            }
+                return true;
+            };
+            int i = 0;
+            if constexpr (FINE)
+                if (chunks > 0 && fine(0)) chunk(i++, std::true_type{});
+            for (; i < chunks; ++i)
+                if (!chunk(i, std::false_type{})) break;
             if (failed && lane == 0) atomicOr(fault, 1u);
         }
     } else {
@@ -634,8 +651,8 @@ bool launch_linear_umma(const nystra::LinArgs& a, cudaStream_t st, cudaError_t* 
         if ((*err = cudaGetSymbolAddress((void**)&fault, nystra::g_fault_linear)) != cudaSuccess) return true;
         for (auto k : {nystra::umma::linear_umma_kernel<false, false>, nystra::umma::linear_umma_kernel<true, false>,
                        nystra::umma::linear_umma_kernel<true, true>}) {
-            if ((*err = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, nystra::umma::kSmem)) !=
-                cudaSuccess)
+            if ((*err = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             nystra::umma::kSmemFine)) != cudaSuccess)
                 return true;
             // the kernels' register shares have to fit what a CTA starts with
             cudaFuncAttributes f;
@@ -657,9 +674,10 @@ bool launch_linear_umma(const nystra::LinArgs& a, cudaStream_t st, cudaError_t* 
         if ((*err = cudaGetLastError()) != cudaSuccess) return true;
         if ((*err = launch_linear_combine(a, st)) != cudaSuccess) return true;
     }
-    auto main = a.N <= nystra::kChunk ? nystra::umma::linear_umma_kernel<true, true>
-                                      : nystra::umma::linear_umma_kernel<true, false>;
-    main<<<grid, nystra::umma::kThreads, nystra::umma::kSmem, st>>>(a, maps, fault);
+    bool fine = a.N <= nystra::kChunk;
+    for (int i = 0; i < a.roles; ++i) fine = fine || !a.role[i].s_in;
+    auto main = fine ? nystra::umma::linear_umma_kernel<true, true> : nystra::umma::linear_umma_kernel<true, false>;
+    main<<<grid, nystra::umma::kThreads, fine ? nystra::umma::kSmemFine : nystra::umma::kSmem, st>>>(a, maps, fault);
     *err = cudaGetLastError();
     return true;
 }

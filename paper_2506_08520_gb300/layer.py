@@ -425,8 +425,10 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_deca
 
     Values have to be finite (behind ``lengths`` anything may lie): one that is not makes
     the results of its 64 tokens and of all later ones of its sequence and head undefined.
-    In 16 bits the state that is returned is summed more exactly than one that is only
-    read on the way, so results with and without ``return_state`` may differ by roundings.
+    In 16 bits the masked scores and the state that meets the queries are rounded on the
+    way, but for the scores of a sequence's first 64 tokens where no state enters it; and the
+    state that is returned is summed more exactly than one that is only read on the way, so
+    results with and without ``return_state`` may differ by roundings.
 
     In a stream capture with ``out`` given the call has no place for a workspace and
     does not split long sequences."""
