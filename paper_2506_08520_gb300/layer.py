@@ -9,8 +9,8 @@ stream or on ``stream``, raise ``ValueError`` for tensors that do not fit and
 
 The calls record no autograd graph: each forward call has its backward call
 beside it, for use inside a ``torch.autograd.Function`` or a training loop of
-one's own.  Inputs that require gradients are refused while grad mode is on,
-rather than silently cut off.
+one's own.  Inputs that require gradients are refused while grad mode is on, and
+inputs with forward-mode tangents always, rather than silently cut off.
 
 A result is allocated on the stream that the call runs on.
 """
@@ -21,6 +21,7 @@ import functools
 import math
 
 import torch
+from torch.autograd import forward_ad
 
 from .binding import _DTYPE_CODE, NYSTRA_OK, NystraError, _stream_ptr, lib
 
@@ -43,18 +44,27 @@ def _array(strides):
     return (ctypes.c_longlong * len(strides))(*strides)
 
 
+def _recorded(t) -> bool:
+    """Whether autograd would record a graph for t, or carry a tangent of it along."""
+    if t.requires_grad and torch.is_grad_enabled():
+        return True
+    # (a Function's forward method is called with tangents that are its jvp method's to carry on)
+    return (forward_ad._current_level >= 0 and torch._C._is_fwd_grad_enabled()
+            and forward_ad.unpack_dual(t).tangent is not None)
+
+
 def _tensors(*ts):
     """Checks that hold for every tensor of a call: one CUDA device, no gradients to record."""
-    grad = torch.is_grad_enabled()
     device = ts[0].get_device()
     for t in ts:
         if t is None:
             continue
         if t.get_device() != device or not t.is_cuda:
             raise ValueError("tensors must be on one CUDA device (no CPU path)")
-        if grad and t.requires_grad:
-            raise ValueError("an input requires gradients, and these calls record no autograd graph: call under "
-                             "torch.no_grad() or in an autograd.Function, with the *_backward call for its gradient")
+        if _recorded(t):
+            raise ValueError("an input requires gradients or has a tangent, and these calls record no autograd graph: "
+                             "call under torch.no_grad() or in an autograd.Function, with the *_backward call for its "
+                             "gradient")
 
 
 def _dtype(*sigs) -> int:

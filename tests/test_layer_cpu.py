@@ -149,3 +149,37 @@ def test_sizes_beyond_32_bits_are_refused(big):
 def test_norm_rows_too_long():
     with pytest.raises(pn.NystraError):
         layer._norm_plan(sig(1, 2 ** 30 + 1), None, None, None, None)
+
+
+def test_gradients_that_would_be_cut_off():
+    """Both kinds: a graph to record, and a tangent that goes along forward."""
+    x = torch.ones(3)
+    assert not layer._recorded(x)
+    g = x.clone().requires_grad_()
+    assert layer._recorded(g)
+    with torch.no_grad():
+        assert not layer._recorded(g)
+    import torch.autograd.forward_ad as fw
+    with fw.dual_level():
+        dual = fw.make_dual(x, x)
+        assert layer._recorded(dual) and not layer._recorded(x)
+        with torch.no_grad():  # which does not stop a tangent
+            assert layer._recorded(dual) == (fw.unpack_dual(dual * 2).tangent is not None)
+        primal = fw.unpack_dual(dual).primal
+        assert not layer._recorded(primal)
+
+        class Twice(torch.autograd.Function):  # of one's own, with its derivatives: fine inside
+            @staticmethod
+            def forward(x):
+                assert not layer._recorded(x)
+                return x * 2
+
+            @staticmethod
+            def setup_context(ctx, inputs, output):
+                pass
+
+            @staticmethod
+            def jvp(ctx, t):
+                return t * 2
+
+        assert fw.unpack_dual(Twice.apply(dual)).tangent.tolist() == [2, 2, 2]
