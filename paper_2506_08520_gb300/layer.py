@@ -226,12 +226,12 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.
 
 
 def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
-                        weight: torch.Tensor | None = None, stream=None):
+                        weight: torch.Tensor | None = None, stream=None, bias: torch.Tensor | None = None):
     """Gradients of ``layer_norm``: ``(dx, dweight, dbias)`` from the output's
     gradient, the input and the saved statistics.  Without ``weight`` the last two
-    are None."""
-    _tensors(dy, x, mean, rstd, weight)
-    dt, wdt, rows, C, xs, _, ds, need = _norm_plan(_sig(x), _sig(weight), None, None, _sig(dy))
+    are None, but for ``dbias`` where ``bias`` is given (which is else not needed)."""
+    _tensors(dy, x, mean, rstd, weight, bias)
+    dt, wdt, rows, C, xs, _, ds, need = _norm_plan(_sig(x), _sig(weight), _sig(bias), None, _sig(dy))
     for t in (mean, rstd):
         if t.shape != x.shape[:-1] or t.dtype != torch.float32 or not t.is_contiguous():
             raise ValueError("mean and rstd must be contiguous fp32 tensors of x's shape without the last axis")
@@ -242,6 +242,8 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, r
         if weight is not None:
             both, ws, wp = _result((2, C), weight, need)
             dw, db = both.unbind(0)
+        elif bias is not None:
+            db, ws, wp = _result((C,), bias, need)
         _raise(lib().nystra_layer_norm_backward(dy.data_ptr(), ds, x.data_ptr(), xs, mean.data_ptr(), rstd.data_ptr(),
                                                 _ptr(weight), dx.data_ptr(), C, _ptr(dw), _ptr(db), rows, C, dt, wdt,
                                                 wp, need, st), "nystra_layer_norm_backward")
