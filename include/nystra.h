@@ -424,7 +424,7 @@ typedef enum {
  *            slices like a fused projection's, sequence by sequence or token
  *            by token or head by head).
  *  inv_freq  [rotary_dim / 2] fp64, finite: radians per position.  Angles are
- *            accurate to about 2^-53 |p inv_freq| + 2^-24 radians.
+ *            accurate to about 2^-52 |p inv_freq| + 2^-62 |p| + 2^-24 radians.
  *  positions [N], or [n, N] with positions_stride elements between sequences
  *            (0: shared): positions_bits is 64 or 32 (signed).  Null: token t
  *            has position t.

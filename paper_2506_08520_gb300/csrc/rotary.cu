@@ -9,7 +9,7 @@
 // rad, and fp64 is slow here.  A frequency is kept as a 64-bit fixed-point
 // fraction of a turn per token, F = 2^64 frac(f / 2 pi), and p F mod 2^64 is
 // the angle's fraction of a turn: an integer product that wraps where the
-// angle does, exact but for F's rounding (that of f / 2 pi in fp64).
+// angle does, exact but for F's rounding (that of f / 2 pi in fp64, and 2^-65 of a turn).
 //
 // Bound by memory: each value is read and written once.  A thread keeps the
 // sines of its pairs for several heads, which all turn alike.  2 x 8192 tokens of
@@ -40,8 +40,10 @@ __global__ void __launch_bounds__(kRotThreads, 4) rotary_kernel(const RotArgs a)
     __shared__ unsigned long long turns[128];
     const int half = a.r / 2;
     for (int i = threadIdx.x; i < half; i += blockDim.x) {
-        const double f = a.inv_freq[i] * 0.15915494309189533577;  // 1 / (2 pi)
-        turns[i] = __double2ull_rn((f - floor(f)) * 18446744073709551616.0);
+        // of a negative frequency's size, then negated: 1 - f would cut a small one off at 2^-54
+        const double f = fabs(a.inv_freq[i]) * 0.15915494309189533577;  // 1 / (2 pi)
+        const unsigned long long t = __double2ull_rn((f - floor(f)) * 18446744073709551616.0);
+        turns[i] = a.inv_freq[i] < 0 ? 0 - t : t;
     }
     __syncthreads();
     const int slot = threadIdx.x % a.slots;
