@@ -357,8 +357,9 @@ NYSTRA_API long long nystra_debug_stages_size(int N, int d_h, int m);
  *           is the memory from its first to its last element: a result's span
  *           must not overlap an input's or another result's (rotary positions
  *           may also be applied in place).
- *  Alignment  pointers are aligned to their element type.  Rows that start on
- *           16-byte boundaries are read in wide words, others element by element.
+ *  Alignment  pointers are aligned to their element type.  Rows are read in the
+ *           widest words (16 bytes at most) on whose boundaries all of them start
+ *           and end, in single elements where there is none.
  *  dtype    q, k, v, x and their results and gradients: fp32, bf16 or fp16;
  *           statistics, decays and attention states are fp32.
  *  Empty    a call whose n, heads, N, rows or C leaves no element to write is
@@ -465,7 +466,8 @@ NYSTRA_API int nystra_rotary(const void* q, const long long* q_strides, void* q_
  * few terms: there the scores carry two parts, and a result is off by its own
  * rounding only.  A call with a state for a single token rounds the state;
  * nystra_linear_attention_step does not.
- * fp32 operands are taken apart into 16-bit parts that carry all of them.
+ * fp32 operands are taken apart into three bf16 parts that carry all of them
+ * (sizes from 2^-109 to below 2^128 (1 - 2^-9), where the first part overflows).
  * Values: finite.  One that is not makes the results of its 64 tokens and of all
  * later ones of its sequence and head undefined (nothing else); behind `lengths`
  * anything may lie.

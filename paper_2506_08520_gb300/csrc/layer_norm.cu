@@ -13,10 +13,13 @@
 // Both directions are bound by memory: 2 (forward) and 3 (backward) elements
 // moved per element, about 8 and 14 operations.  Measured: forward of 262144 rows of
 // 180 in bf16 35 us (5.4 TB/s; loads without copies ahead 46 at 64 registers, 38 at 88),
-// backward of 16384 x 4096 in bf16 94 us a call, 6 of them for the sums (4.3 TB/s).  The backward
-// pass waits for its shuffles and shared memory at 15 warps an SM (two CTAs by registers); xh, formed once
-// a row, takes the registers of x (formed again for dx: 100 us).  Weights in shared memory
-// instead of registers give three CTAs an SM and were slower all the same.
+// backward of 16384 x 4096 in bf16 88 us + 6 for the sums (4.3 TB/s).  The backward
+// pass issues 350 instructions a thread and row at 15 warps an SM (114 registers): 44% of
+// the issue slots, waiting for its shuffles and shared memory.  xh, formed once a row,
+// takes the registers of x (formed again for dx: 6 us more); weights in shared memory
+// instead of registers give three CTAs an SM and were slower all the same (115 us).
+// Rows that do not fit the registers (forward above 8192 values in fp32 and 16384 in 16
+// bits, backward above 8192, less where rows are not aligned) go value by value.
 #include "common.cuh"
 #include "layer.cuh"
 #include "pack.cuh"

@@ -28,7 +28,7 @@
 // A chunk is 48 KB in and 16 KB out, 2800 cycles of one SM's share of the memory, and
 // 900 to 1150 of tensor pipe.  Measured: 3400 cycles (2 parts of w c) to 3950 (3) a
 // chunk; 8 x 16 heads x 4096 tokens of 128 with the final state 132 us, on 128 of
-// 152 SMs; 25% tensor pipe, 48% of issue slots.  Latency binds it: with all 16 warps
+// 152 SMs; 37% tensor pipe, 61% of issue slots on those.  Latency binds it: with all 16 warps
 // in step it took 5200 cycles, with 8 + 8 warps 4400, with the scores on the collecting
 // warps 5400; splitting a block of scores between the kinds of warps cost more than
 // the two blocks that two of the scoring warps have too many.  Without L2

@@ -3,7 +3,8 @@ positions and causal linear attention with a decay per head.
 
 They share the attention calls' layout, ``[n, heads, N, d]``, but take any
 strides on the first three axes (``project_qkv``'s results, token-major tensors,
-slices of a wider projection).  Like the other calls they run on the current
+slices of a wider projection); ``layer_norm`` takes rows of any shape in front that
+one stride steps along.  Like the other calls they run on the current
 stream or on ``stream``, raise ``ValueError`` for tensors that do not fit and
 ``NystraError`` for what the C ABI refuses, and have no CPU path.
 
@@ -12,7 +13,9 @@ beside it, for use inside a ``torch.autograd.Function`` or a training loop of
 one's own.  Inputs that require gradients are refused while grad mode is on, and
 inputs with forward-mode tangents always, rather than silently cut off.
 
-A result is allocated on the stream that the call runs on.
+A result is allocated on the stream that the call runs on.  An input of another
+stream's is not recorded on it (``Tensor.record_stream`` does that): as with torch's
+own calls, it has to be there when the call runs, and to stay until it has.
 """
 from __future__ import annotations
 
