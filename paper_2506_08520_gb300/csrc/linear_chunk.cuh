@@ -310,6 +310,35 @@ __device__ __forceinline__ void store_tile(const T* tile, T* first, long long st
         store_rows<T, DP, THREADS, 2>(tile, first, step, d, cnt);
 }
 
+// Rows behind a sequence: `rows` rows of d zeros, a thread a column piece of every RP-th row.
+template <int THREADS, int BYTES>
+__device__ __forceinline__ void zero_rows(unsigned char* first, long long step, int row_bytes, int rows) {
+    const int per = row_bytes / BYTES, rp = THREADS / per;
+    const int row0 = threadIdx.x / per, piece = threadIdx.x % per;
+    if (row0 >= rp) return;
+    using Raw = typename RawWord<BYTES>::type;
+    unsigned char* to = first + row0 * step + piece * BYTES;
+#pragma unroll 4
+    for (int row = row0; row < rows; row += rp) {
+        *reinterpret_cast<Raw*>(to) = Raw{};
+        to += rp * step;
+    }
+}
+template <typename T, int THREADS>
+__device__ __forceinline__ void zero_tile(T* first, long long step, int d, int rows, int bytes) {
+    unsigned char* const p = reinterpret_cast<unsigned char*>(first);
+    const long long s = step * (long long)sizeof(T);
+    const int n = d * (int)sizeof(T);
+    if (bytes == 16)
+        zero_rows<THREADS, 16>(p, s, n, rows);
+    else if (bytes == 8)
+        zero_rows<THREADS, 8>(p, s, n, rows);
+    else if (sizeof(T) == 4 || bytes == 4)
+        zero_rows<THREADS, 4>(p, s, n, rows);
+    else if constexpr (sizeof(T) == 2)
+        zero_rows<THREADS, 2>(p, s, n, rows);
+}
+
 // ------------------------------------------------------------ the kernel
 // Powers of gamma with their factors, by what they multiply.
 struct ChunkTables {
@@ -462,6 +491,10 @@ linear_chunk_kernel(const __grid_constant__ LinArgs args) {
         if (i < 16 + kChunk) tab.score[i] = i < 16 ? 0.f : r.s_scale * r.o_scale * p;
         if (i < kChunk) tab.inter[i] = r.o_scale * decay.power(i + e0);
         tab.weight[i] = i < kChunk ? r.s_scale * decay.power(kChunk - e0 - i) : 0.f;
+    }
+    if (MAIN) {  // rows behind the sequence (here, so that nothing of it stays in registers over the chunks)
+        const int z0 = max(u0, len);
+        zero_tile<T, THREADS>(out + z0 * r.so.token, r.so.token, r.dc, u1 - z0, r.wo);
     }
 
     // the state: rows row0 + g (+ 8), columns 8 nt + c2 (+ 1)
@@ -682,12 +715,6 @@ linear_chunk_kernel(const __grid_constant__ LinArgs args) {
             store_tile<T, DP, THREADS>(reinterpret_cast<const T*>(ta), po + (long long)i * kChunk * dos, dos, r.dc, cnt,
                                        r.wo);
         }
-    }
-    if (MAIN) {  // rows behind the sequence
-        const int z0 = max(u0, len);
-        const long long n = z0 < u1 ? (long long)(u1 - z0) * r.dc : 0;
-        for (long long i = threadIdx.x; i < n; i += THREADS)
-            out[(z0 + i / r.dc) * r.so.token + i % r.dc] = from_f32<T>(0.f);
     }
     if (!keep) return;
     float* e_out = MAIN ? r.s_out + (long long)unit * r.db * r.dc : lin_ws(args, blockIdx.y, unit, seg);

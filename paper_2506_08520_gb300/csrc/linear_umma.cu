@@ -553,9 +553,8 @@ linear_umma_kernel(const __grid_constant__ LinArgs args, const __grid_constant__
         if (failed && lane == 0) atomicOr(fault, 1u);
         if (MAIN) {  // rows behind the sequence
             const int z0 = max(u0, len);
-            const long long n = z0 < u1 ? (long long)(u1 - z0) * r.dc : 0;
-            for (long long i = threadIdx.x; i < n; i += kCollect)
-                out[(z0 + i / r.dc) * r.so.token + i % r.dc] = from_f32<T>(0.f);
+            zero_rows<kCollect, 16>(reinterpret_cast<unsigned char*>(out + z0 * r.so.token), r.so.token * 2, r.dc * 2,
+                                    u1 - z0);
         }
         if (keep) {
             float* const to = MAIN ? r.s_out + (long long)unit * r.db * r.dc : lin_ws(args, blockIdx.y, unit, seg);
