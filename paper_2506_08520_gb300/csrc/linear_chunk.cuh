@@ -29,8 +29,8 @@
 // Bound by issue and latency: a chunk of 64-feature heads is about 6000 warp
 // instructions and 544 MMAs (650 of the 1400 cycles that its bytes take at the memory's
 // rate, on one SM).  Measured (d = 64, fp16, 8 heads x 65536 tokens in 74 segments each):
-// 85 us for the outputs with four CTAs an SM (with three a fifth more), 38 for the segments'
-// states, 11 to combine them; 51% of issue slots, tensor pipe 42%.
+// 87 us for the outputs with four CTAs an SM (with three a fifth more), 38 for the segments'
+// states, 11 to combine them; 50% of issue slots, tensor pipe 41%.
 #pragma once
 
 #include <type_traits>
